@@ -19,12 +19,14 @@ __device__ __forceinline__ void split_pieces(float a, float b, uint32_t (&p)[N])
 
 // The r rows of W to [piece][dimensions 0 .. 63, 64 .. 127][channel], 128-byte rows, swizzled (K-major): a warp of
 // kWarps per channel, a lane per four dimensions, kRows channels i0, i0 + kWarps, ... at a time: their loads, and
-// what is made of them.  norm(channel, |w|^2) in every lane, where kNorms.
+// what is made of them.  norm(channel, |w|^2) in every lane, where kNorms.  A head without channels has no rows, and
+// its offset need not be one that 16 bytes can be read at.
 template <int kWarps, int kRows>
 __device__ __forceinline__ void load_basis(float4 (&w)[kRows], const float* W, int r, int i0) {
 #pragma unroll
   for (int k = 0; k < kRows; ++k)
-    w[k] = reinterpret_cast<const float4*>(W + max(min(i0 + k * kWarps, r - 1), 0) * kD)[threadIdx.x & 31];
+    w[k] = r > 0 ? reinterpret_cast<const float4*>(W + min(i0 + k * kWarps, r - 1) * kD)[threadIdx.x & 31]
+                 : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 template <int N, int kWarps, bool kNorms, int kRows, typename F>
 __device__ __forceinline__ void lay_basis(unsigned char (*to)[2][kD * 128], const float4 (&w)[kRows], int r, int i0, F norm) {
