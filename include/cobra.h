@@ -514,7 +514,9 @@ cobra_status cobra_tree_workspace_size(const cobra_tree_desc* desc, size_t* byte
  *   o = sum_t p_t V_t / sum_t p_t,  p_t = exp(z_t),  z_t = cap(q . K_t / sqrt(d)) + slope_g (pos_t - p_i)
  * over the cached tokens t < seq_lens[s] (keys and values as in cobra_decode_attn, means included; key t at
  * position t) with p_i - window < t <= p_i, and the drafted tokens j < n_draft[s] whose bit (i, j) of
- * tree_mask is set (within the window too).  A token that sees nothing gets zeros.
+ * tree_mask is set (within the window too).  A token that sees nothing gets zeros; NaN and infinities of
+ * queries, drafted keys and values or slopes reach what sees them as they do in the formula (scores that are not
+ * finite give NaN), and nothing else.
  *   q          device bf16, token i, query head j at q[l*sl + s*ss + i*st + j*128]
  *   k_draft, v_draft  device bf16 (rotated like the cache's keys), or both NULL: queries see the cache
  *              alone (max_draft = 1 is single-token decode)

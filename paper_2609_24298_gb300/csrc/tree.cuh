@@ -10,7 +10,8 @@
 //   bias             z <- z + slope2_g (t - p_i)
 //   seen             p_i - window < t <= p_i, and t below the sequence's length
 // and o_c = sum_t 2^z_t V_t / sum_t 2^z_t, the cached values accumulated in rank space (deviations from
-// the code centre) and mapped back once.  A column that sees nothing gives zeros.
+// the code centre) and mapped back once.  A column that sees nothing gives zeros; one whose scores are not finite
+// (a query, drafted key or slope with a NaN or an infinity, or beyond fp32) gives NaN, as the definition does.
 //
 //   tree_prepare_kernel  per (head, sequence, 32 columns) q~ as f16 with a power-of-two scale, c0, and
 //                        the drafted tokens' own softmax partial; one CTA lays out the scan's work
@@ -35,6 +36,8 @@ constexpr int kTreeMaxDraft = 64;
 constexpr uint64_t kTreeWaitNs = 2000000000ull;  // 2 s
 constexpr int kTreeChunk = 32;    // columns of a prepare unit
 constexpr int kTreePart = kD + 4;  // floats of a column's partial: m, l, -, -, O[128]
+constexpr float kTreeLargest = 1e38f;   // magnitude of a score that fp32 holds with its parts
+constexpr float kTreeLowest = -3e38f;   // stands for a drafted score of -inf: below every other, but seen
 constexpr float kTreeBound = 80.f;  // scores this near their reference need no running maximum: 2^80 times codes of 2^7, summed over 2^31 tokens, is finite
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kInvSqrtD = 0.088388347648318440f;
@@ -45,7 +48,7 @@ struct TreeCol {     // what the scan knows of a column
   float scale;       // 2^-e of the q~ scale
   int lo, hi;        // cached tokens [lo, hi) that it sees
   int bounded;       // scores of the chunk's columns, less their biases, are within kTreeBound of c0 (0 with a cap)
-  int reserved;
+  int bad;           // scores that are not finite: the scan has zeros for the column, the combine makes it NaN
 };
 static_assert(sizeof(TreeCol) == 32, "copied as 16-byte units");
 
@@ -273,6 +276,7 @@ struct TreeProjSmem {
   unsigned char w[2][2][kD * 128], x[2][kTreeChunk * 128];  // operands on 1024-byte boundaries
   float os[kTreeChunk][kTreeProjLd];
   float dot[kTreeChunk], red[2][8];
+  int bad[kTreeChunk];
   unsigned long long done;
   uint32_t tmem;
 };
@@ -363,21 +367,25 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
   if (warp == 0) tmem_dealloc(tmem, kTreeChunk);
   const float f = he.delta * kInvSqrtD * kLog2e;
   // per column: the largest |q~|, how far a score can be from c0 (sum |q~| (2^{b-1} - 1/2), a little more for the
-  // roundings; with a cap from 0: the cap)
+  // roundings; with a cap from 0: the cap).  An element that is not finite makes q . mu such; columns with one are left out.
   float top = 0.f, far = 0.f;
   for (int c = warp; c < nv; c += 8) {
-    float s1 = 0.f;
+    float s1 = 0.f, most = 0.f;
 #pragma unroll
     for (int k = 0; k < kD / 32; ++k) {
       const int i = lane + 32 * k;
       const float x = i < r ? fabsf(sm.os[c][i] * f) : 0.f;
-      top = fmaxf(top, x);
+      most = fmaxf(most, x);
       s1 += x;
     }
 #pragma unroll
     for (int m = 16; m; m >>= 1) s1 += __shfl_xor_sync(0xffffffffu, s1, m);
-    far = fmaxf(far, s1 * ((float)(1 << (he.b > 0 ? he.b - 1 : 0)) - 0.5f) * 1.01f);
-    if (!(s1 < INFINITY)) far = INFINITY;
+    s1 *= ((float)(1 << (he.b > 0 ? he.b - 1 : 0)) - 0.5f) * 1.01f;
+    const bool bad = !(s1 + fabsf(sm.dot[c]) * (kInvSqrtD * kLog2e) < kTreeLargest);
+    if (lane == 0) sm.bad[c] = bad;
+    if (bad) continue;
+    top = fmaxf(top, most);
+    far = fmaxf(far, s1);
   }
   if (__any_sync(0xffffffffu, !(fabsf(slope) < 1e20f))) far = INFINITY;  // (times 2^31 it would not be finite)
 #pragma unroll
@@ -390,7 +398,7 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
   // by 2^-25, which the codes of a head make 2^-11 of a score's log2 unit at most: q~ is scaled only where it
   // would overflow
   int e = 0;
-  if (top >= 32768.f && top < INFINITY) {
+  if (top >= 32768.f) {
     int ex;
     frexpf(top, &ex);
     e = max(15 - ex, -100);
@@ -402,6 +410,7 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
   const int ncol = min(kTreeChunk, a.nc);
   for (int idx = tid; idx < ncol * (kD / 8); idx += 256) {  // 8 places of a column
     const int c = idx / (kD / 8), p = 8 * (idx % (kD / 8));
+    const bool fed = c < nv && !sm.bad[c];
     uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -409,16 +418,18 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int i = tc_k_channel(p + 2 * k + h);
-        x[h] = c < nv && i < r ? sm.os[c][i] * f * up : 0.f;
+        x[h] = fed && i < r ? sm.os[c][i] * f * up : 0.f;
       }
       w[k] = pack_f16(x[0], x[1]);
     }
     *reinterpret_cast<uint4*>(img + tree_img_at(a.nc, cb + c, p)) = make_uint4(w[0], w[1], w[2], w[3]);
   }
   const int bounded = e == 0 && (a.cap2 > 0.f ? a.cap2 <= kTreeBound && far < INFINITY : far <= kTreeBound);
-  if (tid < ncol)
-    a.col[unit * a.nc + cb + tid] =
-        TreeCol{tid < nv ? sm.dot[tid] * (kInvSqrtD * kLog2e) : 0.f, slope, p, ldexpf(1.f, -e), seen.x, seen.y, bounded, 0};
+  if (tid < ncol) {
+    const int bad = tid < nv ? sm.bad[tid] : 0;
+    const float c0f = tid < nv && !bad ? sm.dot[tid] * (kInvSqrtD * kLog2e) : 0.f;
+    a.col[unit * a.nc + cb + tid] = TreeCol{c0f, slope, p, ldexpf(1.f, -e), seen.x, seen.y, bounded, bad};
+  }
 }
 
 // The drafted tokens' own part of 32 columns: m, l and O in the model's dimensions.
@@ -485,7 +496,7 @@ __device__ __forceinline__ void tree_draft_part(const TreeArgs& a, TreeDraftSmem
       float y = z[u >> 1][u & 1];
       if (a.cap2 > 0.f) y = tree_cap(y, a.cap2, k2);
       if (a.slopes) y = fmaf(a.slopes[kv * G + g] * kLog2e, (float)dist, y);
-      sm.z[c][j] = seen ? y : -INFINITY;
+      sm.z[c][j] = !seen ? -INFINITY : y < kTreeLowest ? kTreeLowest : y;
     }
   }
   __syncthreads();
@@ -509,7 +520,7 @@ __device__ __forceinline__ void tree_draft_part(const TreeArgs& a, TreeDraftSmem
   }
   __syncthreads();
   // values: a thread has one dimension of 16 columns.  A token that a column does not see has p = 0,
-  // whatever its value is; one that no column sees is passed over.
+  // whatever its value is.
   const int d = tid & 127, cb = 16 * (tid >> 7);
   float o[16] = {};
   for (int j = 0; j < n; ++j) {
@@ -522,7 +533,7 @@ __device__ __forceinline__ void tree_draft_part(const TreeArgs& a, TreeDraftSmem
       for (int k = 0; k < 16; ++k) o[k] = fmaf(p[k], v, o[k]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 16; ++k) o[k] = p[k] == 0.f ? o[k] : fmaf(p[k], v, o[k]);
+      for (int k = 0; k < 16; ++k) o[k] = cb + k >= nv || sm.z[cb + k][j] == -INFINITY ? o[k] : fmaf(p[k], v, o[k]);
     }
   }
 #pragma unroll
@@ -740,7 +751,7 @@ __device__ __forceinline__ float tree_reduce(float (&v)[N], Op op) {
   return v[0];
 }
 // Scores of the thread's token against the columns: absolute (log2 units) or less the reference.  A column
-// without a reference has sub = +1e30 (plain) or -1e30 (ref), so that any score it sees asks for one.
+// without a reference has sub = +3e38 (plain) or -3e38 (ref), so that any score it sees asks for one.
 template <int NCW, bool ABS>
 __device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>& w, const uint32_t (&x)[NCW], float sc,
                                             float k2, bool plain, bool masked, int tok, float (&z)[NCW]) {
@@ -1042,7 +1053,7 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
         // (the first one where the slope is negative)
         const float mid = a.cap2 > 0.f ? 0.f : c.c0;
         const int at = c.slope2 < 0.f ? c.lo : c.hi - 1;
-        w.sub[t] = plain ? 1e30f : c.bounded ? mid : -1e30f;
+        w.sub[t] = plain ? -kTreeLowest : c.bounded ? mid : kTreeLowest;
         w.ref[t] = !c.bounded ? -INFINITY : a.slopes ? fmaf(c.slope2, (float)((long long)at - c.pos), mid) : mid;
         w.slope[t] = c.slope2;
         w.pos[t] = c.bounded ? at : c.pos;
@@ -1339,6 +1350,8 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs a) {
   }
   if (warp < live) {
     const float2 dr = draft ? *reinterpret_cast<const float2*>(draft + warp * kTreePart) : make_float2(-INFINITY, 0.f);
+    const TreeCol* col = a.col + unit * a.nc + (c0 + warp) % a.nc;
+    const int cached = col->hi > col->lo, bad = col->bad;
     float M = dr.x, l = 0.f;
     constexpr int kAt = kTreeParts / 32;
     float2 ml[kAt];
@@ -1352,19 +1365,22 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs a) {
     for (int x = 16; x; x >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, x));
 #pragma unroll
     for (int k = 0; k < kAt; ++k) {
-      const float e = ml[k].x == -INFINITY ? 0.f : exp2f(ml[k].x - M);
-      if (e > 0.f) l = fmaf(e, ml[k].y, l);
+      const float e = ml[k].y == 0.f ? 0.f : exp2f(ml[k].x - M);
+      l = fmaf(e, ml[k].y, l);  // (a sum that is not finite stays so)
       ml[k].x = e;
     }
 #pragma unroll
     for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-    const float wd = dr.x == -INFINITY ? 0.f : exp2f(dr.x - M);
-    const float sum = l + (wd > 0.f ? wd * dr.y : 0.f), inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float wd = dr.y == 0.f ? 0.f : exp2f(dr.x - M);
+    const float sum = fmaf(wd, dr.y, l);
+    // NaN: the combined scores are not finite, all of them are -inf, or their sum is not a number
+    const float inv = !cached && dr.y == 0.f ? 0.f
+                      : bad || M <= kTreeLowest || !(sum > 0.f && sum < INFINITY) ? __int_as_float(0x7fffffff) : 1.f / sum;
 #pragma unroll
     for (int k = 0; k < kAt; ++k)
       if (lane + 32 * k < np) wt[warp][lane + 32 * k] = ml[k].x * inv;
     if (lane == 0) {
-      wd_s[warp] = wd * inv;
+      wd_s[warp] = dr.y == 0.f ? -1.f : wd * inv;  // (a value that is not finite shows whatever its weight)
       pc_s[warp] = l * inv;
     }
   }
@@ -1413,7 +1429,7 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(TreeArgs a) {
 #pragma unroll
     for (int w = 0; w < 8; ++w) y += sums[w][c8][dim];
     y = fmaf(mu, pc_s[c8], y);
-    if (wd_s[c8] > 0.f) y = fmaf(dv[k], wd_s[c8], y);
+    if (wd_s[c8] >= 0.f) y = fmaf(dv[k], wd_s[c8], y);
     a.out[layer * a.o_sl + (long long)s * a.o_ss + (long long)(col / G) * a.o_st + (kv * G + col % G) * kD + dim] = __float2bfloat16_rn(y);
   }
 }
