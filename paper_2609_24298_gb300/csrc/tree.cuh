@@ -45,9 +45,10 @@ constexpr float kInvSqrtD = 0.088388347648318440f;
 struct TreeCol {     // what the scan knows of a column
   float c0, slope2;
   int pos;
-  float scale;       // 2^-e of the q~ scale
+  float scale;       // 2^-e, if 2^e scales the column's q~
   int lo, hi;        // cached tokens [lo, hi) that it sees
-  int bounded;       // scores of the chunk's columns, less their biases, are within kTreeBound of c0 (0 with a cap)
+  int bounded;       // 1: scores of the chunk's columns, less their biases, are within kTreeBound of c0 (0 with a cap);
+                     // -1: not so, and some of its columns are scaled
   int bad;           // scores that are not finite: the scan has zeros for the column, the combine makes it NaN
 };
 static_assert(sizeof(TreeCol) == 32, "copied as 16-byte units");
@@ -276,7 +277,7 @@ struct TreeProjSmem {
   unsigned char w[2][2][kD * 128], x[2][kTreeChunk * 128];  // operands on 1024-byte boundaries
   float os[kTreeChunk][kTreeProjLd];
   float dot[kTreeChunk], red[2][8];
-  int bad[kTreeChunk];
+  int bad[kTreeChunk], exp[kTreeChunk];  // not finite; exponent of the scale
   unsigned long long done;
   uint32_t tmem;
 };
@@ -382,28 +383,26 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
     for (int m = 16; m; m >>= 1) s1 += __shfl_xor_sync(0xffffffffu, s1, m);
     s1 *= ((float)(1 << (he.b > 0 ? he.b - 1 : 0)) - 0.5f) * 1.01f;
     const bool bad = !(s1 + fabsf(sm.dot[c]) * (kInvSqrtD * kLog2e) < kTreeLargest);
-    if (lane == 0) sm.bad[c] = bad;
+#pragma unroll
+    for (int m = 16; m; m >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, m));
+    // f16 rounds an element by 2^-11 of it (finer than the bf16 query's own 2^-8) down to 2^-14, and smaller ones
+    // by 2^-25, which the codes of a head make 2^-11 of a score's log2 unit at most: a column's q~ is scaled only
+    // where it would overflow
+    if (lane == 0) {
+      int ex = 15;
+      if (!bad && most >= 32768.f) frexpf(most, &ex);
+      sm.bad[c] = bad;
+      sm.exp[c] = 15 - ex;
+    }
     if (bad) continue;
     top = fmaxf(top, most);
     far = fmaxf(far, s1);
   }
   if (__any_sync(0xffffffffu, !(fabsf(slope) < 1e20f))) far = INFINITY;  // (times 2^31 it would not be finite)
-#pragma unroll
-  for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
   if (lane == 0) sm.red[0][warp] = top, sm.red[1][warp] = far;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < 8; ++w) top = fmaxf(top, sm.red[0][w]), far = fmaxf(far, sm.red[1][w]);
-  // f16 rounds an element by 2^-12 of it (finer than the bf16 query's own 2^-9) down to 2^-14, and smaller ones
-  // by 2^-25, which the codes of a head make 2^-11 of a score's log2 unit at most: q~ is scaled only where it
-  // would overflow
-  int e = 0;
-  if (top >= 32768.f) {
-    int ex;
-    frexpf(top, &ex);
-    e = max(15 - ex, -100);
-  }
-  const float up = ldexpf(1.f, e);
   const long long unit = ((long long)head * a.n_seqs + s) * a.tiles + c0 / a.nc;
   const int cb = c0 % a.nc;  // the chunk's first column in its tile
   unsigned char* img = a.img + unit * (2 * a.nc * 128);
@@ -411,6 +410,7 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
   for (int idx = tid; idx < ncol * (kD / 8); idx += 256) {  // 8 places of a column
     const int c = idx / (kD / 8), p = 8 * (idx % (kD / 8));
     const bool fed = c < nv && !sm.bad[c];
+    const float up = fed ? ldexpf(f, sm.exp[c]) : 0.f;
     uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -418,17 +418,17 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int i = tc_k_channel(p + 2 * k + h);
-        x[h] = fed && i < r ? sm.os[c][i] * f * up : 0.f;
+        x[h] = fed && i < r ? sm.os[c][i] * up : 0.f;
       }
       w[k] = pack_f16(x[0], x[1]);
     }
     *reinterpret_cast<uint4*>(img + tree_img_at(a.nc, cb + c, p)) = make_uint4(w[0], w[1], w[2], w[3]);
   }
-  const int bounded = e == 0 && (a.cap2 > 0.f ? a.cap2 <= kTreeBound && far < INFINITY : far <= kTreeBound);
+  const int bounded = top >= 32768.f ? -1 : a.cap2 > 0.f ? a.cap2 <= kTreeBound && far < INFINITY : far <= kTreeBound;
   if (tid < ncol) {
     const int bad = tid < nv ? sm.bad[tid] : 0;
     const float c0f = tid < nv && !bad ? sm.dot[tid] * (kInvSqrtD * kLog2e) : 0.f;
-    a.col[unit * a.nc + cb + tid] = TreeCol{c0f, slope, p, ldexpf(1.f, -e), seen.x, seen.y, bounded, bad};
+    a.col[unit * a.nc + cb + tid] = TreeCol{c0f, slope, p, ldexpf(1.f, tid < nv ? -sm.exp[tid] : 0), seen.x, seen.y, bounded, bad};
   }
 }
 
@@ -646,7 +646,7 @@ template <int NCW>
 struct alignas(16) TreeWg {  // per softmax warpgroup
   float c0[NCW], sub[NCW];     // c0, and what is subtracted from a score: the reference (sub: c0 - reference, plain)
   float ref[NCW], alpha[NCW];
-  float slope[NCW];
+  float slope[NCW], sc[NCW];
   int pos[NCW], lo[NCW], hi[NCW];
   float red[4][NCW];
 };
@@ -753,22 +753,22 @@ __device__ __forceinline__ float tree_reduce(float (&v)[N], Op op) {
 // Scores of the thread's token against the columns: absolute (log2 units) or less the reference.  A column
 // without a reference has sub = +3e38 (plain) or -3e38 (ref), so that any score it sees asks for one.
 template <int NCW, bool ABS>
-__device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>& w, const uint32_t (&x)[NCW], float sc,
-                                            float k2, bool plain, bool masked, int tok, float (&z)[NCW]) {
+__device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>& w, const uint32_t (&x)[NCW], float k2,
+                                            bool plain, bool masked, int tok, float (&z)[NCW]) {
   if (plain) {
     const float* add = ABS ? w.c0 : w.sub;
-    const f32x2 sc2 = pack2(sc, sc);
+    const f32x2 one = pack2(1.f, 1.f);
 #pragma unroll
     for (int j = 0; j < NCW; j += 4) {
       const float4 c = *reinterpret_cast<const float4*>(add + j);
-      const float2 y0 = unpack2(fma2(pack2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), sc2, pack2(c.x, c.y)));
-      const float2 y1 = unpack2(fma2(pack2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), sc2, pack2(c.z, c.w)));
+      const float2 y0 = unpack2(fma2(pack2(__uint_as_float(x[j]), __uint_as_float(x[j + 1])), one, pack2(c.x, c.y)));
+      const float2 y1 = unpack2(fma2(pack2(__uint_as_float(x[j + 2]), __uint_as_float(x[j + 3])), one, pack2(c.z, c.w)));
       z[j] = y0.x, z[j + 1] = y0.y, z[j + 2] = y1.x, z[j + 3] = y1.y;
     }
   } else {
 #pragma unroll
     for (int j = 0; j < NCW; ++j) {
-      float y = fmaf(__uint_as_float(x[j]), sc, w.c0[j]);
+      float y = __uint_as_float(x[j]) + w.c0[j];
       if (a.cap2 > 0.f) y = tree_cap(y, a.cap2, k2);
       if (a.slopes) y = fmaf(w.slope[j], (float)(tok - w.pos[j]), y);
       z[j] = ABS ? y : y - w.sub[j];
@@ -1046,6 +1046,7 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
       if (!ok || !more) break;
       const TreeCol* col = sm.col[seg & 1] + wg * NCW;
       const int live = min(NCW, d.n_col - wg * NCW);  // may be <= 0
+      const bool bounded = col[0].bounded > 0;
       if (t < NCW) {
         const TreeCol c = col[t];
         w.c0[t] = c.c0;
@@ -1053,15 +1054,14 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
         // (the first one where the slope is negative)
         const float mid = a.cap2 > 0.f ? 0.f : c.c0;
         const int at = c.slope2 < 0.f ? c.lo : c.hi - 1;
-        w.sub[t] = plain ? -kTreeLowest : c.bounded ? mid : kTreeLowest;
-        w.ref[t] = !c.bounded ? -INFINITY : a.slopes ? fmaf(c.slope2, (float)((long long)at - c.pos), mid) : mid;
+        w.sub[t] = plain ? -kTreeLowest : bounded ? mid : kTreeLowest;
+        w.ref[t] = !bounded ? -INFINITY : a.slopes ? fmaf(c.slope2, (float)((long long)at - c.pos), mid) : mid;
         w.slope[t] = c.slope2;
-        w.pos[t] = c.bounded ? at : c.pos;
+        w.sc[t] = c.scale;
+        w.pos[t] = bounded ? at : c.pos;
         w.lo[t] = c.lo;
         w.hi[t] = c.hi;
       }
-      const float sc = col[0].scale;
-      const bool bounded = col[0].bounded;
       // rows [lo, hi) are seen whole by every live column
       int lo = 0, hi = 0x7fffffff;
       for (int j = 0; j < live; ++j) lo = max(lo, col[j].lo), hi = min(hi, col[j].hi);
@@ -1144,6 +1144,10 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
           if (d.rk > 0) {
             tree_ld<NCW>(tmem + lanes + kS + 64 * u + wg * NCW, x);
             tree_wait_ld<NCW>(x);
+            if (col[0].bounded < 0) {
+#pragma unroll
+              for (int j = 0; j < NCW; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * w.sc[j]);
+            }
           } else {
 #pragma unroll
             for (int j = 0; j < NCW; ++j) x[j] = 0u;
@@ -1151,7 +1155,7 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
           use(x);
         };
         auto scores = [&](auto abs) {
-          load([&](const uint32_t(&x)[NCW]) { tree_scores<NCW, decltype(abs)::value>(a, w, x, sc, k2, plain, masked, tok, z); });
+          load([&](const uint32_t(&x)[NCW]) { tree_scores<NCW, decltype(abs)::value>(a, w, x, k2, plain, masked, tok, z); });
         };
         float top = -INFINITY;
         if (bounded && plain) {
