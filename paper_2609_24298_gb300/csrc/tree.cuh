@@ -154,10 +154,20 @@ __device__ __forceinline__ int2 tree_seen(const TreeArgs& a, long long p, int T)
 __device__ __forceinline__ int tree_img_at(int nc, int col, int p) {
   return (p >> 6) * nc * 128 + col * 128 + ((((p & 63) >> 3) ^ (col & 7)) << 4) + (p & 7) * 2;
 }
-// z with the cap: cap2 tanh(z / cap2) = cap2 (1 - 2 / (1 + e^{2 z / cap2})).  The difference loses
-// relative, not absolute accuracy near 0: the score is within 2^-22 cap2, far below what a softmax sees.
-__device__ __forceinline__ float tree_cap(float z, float cap2, float k) {  // k = 2 log2e / cap2
+// z with the cap: cap2 tanh(z / cap2) = cap2 (1 - 2 / (1 + e^{2 z / cap2})).  The difference loses relative, not
+// absolute accuracy near 0: the score is within 2^-20 cap2, for caps up to kTreeBound 2^-13 of a log2 unit.
+__device__ __forceinline__ float tree_cap(float z, float cap2, float k) {  // cap2 <= kTreeBound, k = tree_cap_k
   return cap2 - __fdividef(2.f * cap2, 1.f + ex2_approx(z * k));
+}
+__device__ __forceinline__ float tree_cap_k(float cap2) {  // 2 log2e / cap2, finite (0 times it has to be 0)
+  return cap2 > 0.f ? fminf(__fdiv_rn(2.f * kLog2e, cap2), 3e38f) : 0.f;
+}
+// The same for any cap (with one of 1e5 the above would be off by 0.1): below 0.3 cap2 the series of tanh to x^9, whose
+// rest is below 2^-24 of it, so that the result is within 2^-19 of itself.
+__device__ __forceinline__ float tree_cap_any(float z, float cap2, float k) {
+  const float x = z * k * (0.5f / kLog2e), x2 = x * x;
+  const float series = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+  return fabsf(x) < 0.3f ? z * series : tree_cap(z, cap2, k);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -471,7 +481,7 @@ __device__ __forceinline__ void tree_draft_part(const TreeArgs& a, TreeDraftSmem
   }
   __syncthreads();
   // scores: a warp has four columns, its lanes the drafted tokens lane and lane + 32
-  const float k2 = a.cap2 > 0.f ? 2.f * kLog2e / a.cap2 : 0.f;
+  const float k2 = tree_cap_k(a.cap2);
   {
     float z[4][2] = {};
     const int j0 = min(lane, n - 1), j1 = min(lane + 32, n - 1), cw = 4 * warp;
@@ -494,7 +504,7 @@ __device__ __forceinline__ void tree_draft_part(const TreeArgs& a, TreeDraftSmem
       const long long dist = (long long)sm.pos[j] - sm.pos[i];
       const bool seen = (sm.mask[i] >> j & 1ull) != 0ull && (a.window <= 0 || dist > -(long long)a.window);
       float y = z[u >> 1][u & 1];
-      if (a.cap2 > 0.f) y = tree_cap(y, a.cap2, k2);
+      if (a.cap2 > 0.f) y = tree_cap_any(y, a.cap2, k2);
       if (a.slopes) y = fmaf(a.slopes[kv * G + g] * kLog2e, (float)dist, y);
       sm.z[c][j] = !seen ? -INFINITY : y < kTreeLowest ? kTreeLowest : y;
     }
@@ -752,7 +762,7 @@ __device__ __forceinline__ float tree_reduce(float (&v)[N], Op op) {
 }
 // Scores of the thread's token against the columns: absolute (log2 units) or less the reference.  A column
 // without a reference has sub = +3e38 (plain) or -3e38 (ref), so that any score it sees asks for one.
-template <int NCW, bool ABS>
+template <int NCW, bool ABS, bool BOUNDED>
 __device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>& w, const uint32_t (&x)[NCW], float k2,
                                             bool plain, bool masked, int tok, float (&z)[NCW]) {
   if (plain) {
@@ -769,7 +779,7 @@ __device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>
 #pragma unroll
     for (int j = 0; j < NCW; ++j) {
       float y = __uint_as_float(x[j]) + w.c0[j];
-      if (a.cap2 > 0.f) y = tree_cap(y, a.cap2, k2);
+      if (a.cap2 > 0.f) y = BOUNDED ? tree_cap(y, a.cap2, k2) : tree_cap_any(y, a.cap2, k2);
       if (a.slopes) y = fmaf(w.slope[j], (float)(tok - w.pos[j]), y);
       z[j] = ABS ? y : y - w.sub[j];
     }
@@ -1034,7 +1044,7 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
     const uint32_t lanes = (uint32_t)(32 * wq) << 16;
     TreeWg<NCW>& w = sm.wg[wg];
     const bool plain = !(a.cap2 > 0.f) && !a.slopes;
-    const float k2 = a.cap2 > 0.f ? 2.f * kLog2e / a.cap2 : 0.f;
+    const float k2 = tree_cap_k(a.cap2);
     int n = 0, pb = 0, ph = 1;  // row, its buffer of P and the phase of the buffer's last product
     arrive(sm.s_ready[0]);  // both buffers of S are free
     arrive(sm.s_ready[1]);
@@ -1154,8 +1164,10 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
           }
           use(x);
         };
-        auto scores = [&](auto abs) {
-          load([&](const uint32_t(&x)[NCW]) { tree_scores<NCW, decltype(abs)::value>(a, w, x, k2, plain, masked, tok, z); });
+        auto scores = [&](auto abs, auto bnd) {
+          load([&](const uint32_t(&x)[NCW]) {
+            tree_scores<NCW, decltype(abs)::value, decltype(bnd)::value>(a, w, x, k2, plain, masked, tok, z);
+          });
         };
         float top = -INFINITY;
         if (bounded && plain) {
@@ -1168,16 +1180,16 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
             for (int j = 0; j < NCW; ++j)
               if (tok < w.lo[j] || tok >= w.hi[j]) z[j] = -INFINITY;
           }
+        } else if (bounded) {
+          scores(std::false_type{}, std::true_type{});
         } else {
-          scores(std::false_type{});
-          if (!bounded) {
+          scores(std::false_type{}, std::false_type{});
 #pragma unroll
-            for (int j = 0; j < NCW; ++j) top = fmaxf(top, z[j]);
-          }
+          for (int j = 0; j < NCW; ++j) top = fmaxf(top, z[j]);
         }
         if (!bounded && wg_any(wg, top > kTreeTau)) {
           // the columns' maxima over the row, new references where they are exceeded
-          scores(std::true_type{});
+          scores(std::true_type{}, std::false_type{});
           const float mine = tree_reduce<NCW>(z, [](float p, float q) { return fmaxf(p, q); });
           w.red[wq][tree_owned<NCW>(lane)] = mine;
           wg_sync(wg);
@@ -1208,7 +1220,7 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
             }
             tc_wait_st();
           }
-          scores(std::false_type{});
+          scores(std::false_type{}, std::false_type{});
         }
         tc_fence_before();
         arrive(sm.s_ready[u]);  // for the row after the next
