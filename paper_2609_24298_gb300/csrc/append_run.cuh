@@ -8,13 +8,13 @@
 // neither on the order of summation nor on how tokens are grouped.
 //
 // The projection: W = w1 + w2 + w3, a turned x = x1 + x2 + x3 in bf16 pieces (each the rounding of what the ones
-// before leave: 2^-27 of a value is left behind), a plain x is bf16 already; the products w_i x_j with i + j <= 4
+// before leave: 2^-26 of a value is left behind), a plain x is bf16 already; the products w_i x_j with i + j <= 4
 // (w_i x_1) accumulate in fp32, the small ones first.  M = 128 channels, N = up to 128 vectors, K = 128.
 // A sum of 16 products and the accumulator keeps bits down to 2^-25 of its largest addend and is cut to 24 bits
 // (measured; addends 1 and s, s = 2^-16 .. 2^-31), so an instruction is off by at most (16 2^-25 + 2^-23) |w| |x|
 // (Cauchy-Schwarz), the last eight make 1.25 2^-18 |w| |x| of it and the ones before, of sums below 2^-7 of
-// that, little.  With the pieces' rest, the turned x (6 2^-24 (|xa| + |xb|) per element) and the rounding of
-// W^T mu that is below 2^-17 (|w| |x| + |W^T mu|); at worst 2^-20.8 |w| |x| was seen (40 x 8192 sums, heavy tails).
+// that, little.  With the pieces' rest and the turned x (6 2^-24 (|xa| + |xb|) per element) that is below
+// 2^-17 |w| |x|, and W^T mu adds its rounding, 2^-24 of it; at worst 2^-20.8 |w| |x| was seen (40 x 8192 sums, heavy tails).
 //
 // A CTA works through its share of all (side, layer, kv head, code row): it lays a head's
 // basis out in pieces, takes rows of up to kTokens tokens together (all new tokens of a sequence in one code row go
@@ -37,19 +37,28 @@ namespace cobra {
 // Long runs: 128 tokens per batch (a whole code row), one CTA per SM.
 struct RunMany {
   static constexpr int kThreads = 512, kTokens = 128, kPieces = 3, kPerSm = 1;
-  static constexpr float kError = 7.63e-6f;  // 2^-17, see above
 };
-// Shorter ones: 64 or 32 tokens per batch, and W and x in two pieces (2^-18 each and the dropped w2 x2 on top of the
-// sums' error: 2^-15.5), so that two CTAs fit: one's products run beside the other's loads, and the next call's
-// basis is laid out while this one still runs.
+// Shorter ones: 64 or 32 tokens per batch, and W and x in two pieces, so that two CTAs fit: one's products run beside
+// the other's loads, and the next call's basis is laid out while this one still runs.
 struct RunMid {
   static constexpr int kThreads = 256, kTokens = 64, kPieces = 2, kPerSm = 2;
-  static constexpr float kError = 2.16e-5f;
 };
 struct RunFew {
   static constexpr int kThreads = 256, kTokens = 32, kPieces = 2, kPerSm = 2;
-  static constexpr float kError = 2.16e-5f;
 };
+// The error of a projection is below 2^-18 |x| times the root of a sum over the channel's basis,
+//   f.x |w|^2 + f.y |w2|^2 + f.z |w - w1 - w2|^2   (the first term alone with three pieces: 2^-17 |w| |x|).
+// With two pieces, in units of 2^-18 |x|: the sums' 1.27 |w|; 2^18 |w - w1 - w2|; and for a turned x what its second piece
+// leaves, 2 |w|, the turn's 0.2 |w| and the dropped w2 x2, 2^10 |w2| (x2 is 2^-8 of x at most, and so may w2 be of w;
+// as a rule it is a third of that, and a bound for the worst case would send 1.7 times as many codes to be done again:
+// 131 us for 129, 32 layers x 64 sequences x 4 tokens).  By Cauchy-Schwarz
+// (a + b + c)^2 <= a^2 / A + b^2 / B + c^2 / C where A + B + C = 1, best with A, B, C as the terms are.
+template <class C>
+__device__ __forceinline__ float3 run_error(bool turn) {
+  if (C::kPieces == 3) return make_float3(4.f, 0.f, 0.f);
+  return turn ? make_float3(3.48f * 3.48f / 0.64f, 1.01f * 1048576.f / 0.24f, 68719476736.f / 0.12f)
+              : make_float3(1.27f * 1.27f / 0.66f, 0.f, 68719476736.f / 0.34f);
+}
 constexpr int kRunSegs = 32;             // code rows per batch
 constexpr int kRunSeqs = 256;            // sequences per block of the row count
 constexpr int kRunCodeLd = 132;
@@ -75,7 +84,7 @@ struct RunSmem {
   // operands: [piece][dimensions 0 .. 63, 64 .. 127][channel or vector] 128-byte rows, swizzled
   unsigned char w[C::kPieces][2][kD * 128], x[C::kPieces][2][C::kTokens * 128];
   uint8_t codes[C::kTokens * kRunCodeLd];
-  float wmu[kD], wnorm[kD];
+  float wmu[kD], werr[kD];  // W^T mu; the projection's error over |x|
   float xnorm[C::kTokens];
   int pre[kRunSeqs + 1];  // rows of the block's sequences before each
   int pos[kRunSeqs], n[kRunSeqs];  // their runs
@@ -220,17 +229,17 @@ __device__ __forceinline__ float run_close(const RunArgs& a, const __nv_bfloat16
   return hi + lo;
 }
 
-// The head's basis in pieces, W^T mu and the columns' norms, by all warps but the first.
+// The head's basis in pieces, W^T mu and the columns' errors, by all warps but the first.
 template <class C>
-__device__ __forceinline__ void run_basis(RunSmem<C>& sm, const float* pool, const HeadEntry& he) {
+__device__ __forceinline__ void run_basis(RunSmem<C>& sm, const float* pool, const HeadEntry& he, bool turn) {
   const int lane = threadIdx.x & 31, i = threadIdx.x - 32;
   if (i < he.r) sm.wmu[i] = pool[he.wmu_off + i];
   constexpr int kWarps = C::kThreads / 32 - 1, kRows = 9;  // rows in flight
   float4 w[kRows];
   for (int i0 = i >> 5; i0 < he.r; i0 += kRows * kWarps) {
     load_basis<kWarps>(w, pool + he.w_off, he.r, i0);
-    lay_basis<C::kPieces, kWarps, true>(sm.w, w, he.r, i0, [&](int ch, float n2) {
-      if (lane == 0) sm.wnorm[ch] = sqrtf(n2);
+    lay_basis<C::kPieces, kWarps, true>(sm.w, w, he.r, i0, run_error<C>(turn), [&](int ch, float n2) {
+      if (lane == 0) sm.werr[ch] = 3.8147e-6f * sqrtf(n2);
     });
   }
 }
@@ -333,8 +342,8 @@ __device__ __forceinline__ bool run_codes(const RunArgs& a, RunSmem<C>& sm, uint
   tc_fence_after();
   // u = y / Delta + 2^{b-1} adds two roundings of a value below 2^{b+1} to the error
   const float half = (float)(1 << (b - 1)), inv_delta = he.inv_delta, top = (float)((1 << b) - 1);
-  auto slack = [&](int ch) { return C::kError * inv_delta * sm.wnorm[ch]; };
-  auto least = [&](int ch) { return C::kError * inv_delta * fabsf(sm.wmu[ch]) + 4.8e-7f * (top + 1.f); };
+  auto slack = [&](int ch) { return inv_delta * sm.werr[ch]; };
+  auto least = [&](int ch) { return 2.4e-7f * inv_delta * fabsf(sm.wmu[ch]) + 4.8e-7f * (top + 1.f); };
   const int blocks = (r + 31) / 32, block = warp & 3, v0 = 32 * (warp >> 2), i = 32 * block + lane;
   if (block < blocks && v0 < nv) {  // the lane's channel, 32 vectors
     const int ch = min(i, r - 1);
@@ -505,7 +514,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kPerSm) append_run_kernel(RunA
   const int hs0 = (int)(2LL * heads * blockIdx.x / gridDim.x);
   HeadEntry he = {};
   bool known = entry(hs0, he);
-  if (warp > 0 && he.r > 0) run_basis(sm, pool, he);
+  if (warp > 0 && he.r > 0) run_basis(sm, pool, he, hs0 < heads && a.table);
   // the tokens, positions and the cache may be produced or read by the kernels ahead
   grid_dep_wait();
   int held = 0, sum = 0;  // the block of sequences that lies in shared memory, its code rows
@@ -585,7 +594,7 @@ __global__ void __launch_bounds__(C::kThreads, C::kPerSm) append_run_kernel(RunA
           if (lane == __popc(taken) - 1) sm.n_vec = sum_n;
           if (lane == 0) sm.n_seg = __popc(taken);
         } else if (fresh) {
-          run_basis(sm, pool, he);
+          run_basis(sm, pool, he, turn);
         }
         fresh = false;
         __syncthreads();

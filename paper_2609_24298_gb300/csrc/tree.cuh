@@ -331,7 +331,7 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
     xa[k] = xb[k] = 0u;
     if (warp + 8 * k < nv) load_pairs(q + (long long)(c / G) * a.q_st + c % G * kD, wide, xa[k], xb[k]);
   }
-  lay_basis<2, 8, false>(sm.w, basis, r, warp, [](int, float) {});
+  lay_basis<2, 8, false>(sm.w, basis, r, warp, float3{}, [](int, float) {});
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     const int c = warp + 8 * k;
