@@ -190,8 +190,8 @@ cobra_status cobra_plan_layout(int n_heads, const int* r, const int* b, long lon
  *
  * cobra_params_build and cobra_params_upload return with the block in place.  A block (or a plan's
  * workspace) that a kernel of the caller's writes must not be written by the kernel directly ahead
- * of cobra_append or a cobra_decode_* call in the stream: these read it while that kernel finishes.
- * cobra_compress reads it in plain stream order.
+ * of cobra_append, cobra_append_tokens or a cobra_decode_* call in the stream: these read it while that
+ * kernel finishes.  cobra_compress and cobra_tree_attn read it in plain stream order.
  * ------------------------------------------------------------------------------------- */
 
 /* Bytes needed for a parameter block of n_heads heads with ranks r (host [n_heads]). */
@@ -483,7 +483,8 @@ typedef struct {
  * sequences of a call may write the same row.  What
  * does not fit - positions outside the cache, counts outside 0 .. max_new, an index outside 0 .. n_src - 1, a
  * head the block does not hold, a position past the table (turned by the last angles) - is skipped and
- * reported through the device status word (cobra_check returns COBRA_EINVAL).  Errors: EINVAL, EALIGN
+ * reported through the device status word (cobra_check returns COBRA_EINVAL).  The block must not be written by
+ * the kernel directly ahead in the stream (all other inputs may be).  Errors: EINVAL, EALIGN
  * (params and cache 256 bytes, table 16), ECUDA. */
 cobra_status cobra_append_tokens(const void* params, const cobra_append_desc* desc, const void* k, const void* v,
                                  const int* pos, const int* n_new, const int* index, const double* rope_table,

@@ -298,6 +298,9 @@ struct TreeProjSmem {
 __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm, int head, int s, int chunk) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   bool known;
+  // ahead of the parameters too: the kernel ahead may write them, and asking for them earlier gained nothing (the
+  // smallest call takes 22.4 us either way)
+  grid_dep_wait();
   const HeadEntry he = tree_head(a, a.k_head0, head, known);
   const float* pool = param_pool(a.block);
   const float* mu = pool + he.mu_off;
@@ -305,9 +308,8 @@ __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm
   float m4[4];  // the lane's dimensions: 2 l, 2 l + 1 and the ones 64 behind
 #pragma unroll
   for (int k = 0; k < 4; ++k) m4[k] = known ? mu[2 * lane + (k & 1) + 64 * (k >> 1)] : 0.f;
-  float4 basis[kD / 8];  // on its way while the call ahead ends and the queries come
+  float4 basis[kD / 8];  // on its way while the queries come
   load_basis<8>(basis, pool + he.w_off, r, warp);
-  grid_dep_wait();
   const int T = tree_len(a, s, false), n = tree_drafts(a, s, false);
   const int c0 = chunk * kTreeChunk, nv = max(0, min(kTreeChunk, n * G - c0));
   if (c0 / a.nc * a.nc >= n * G) return;  // nobody reads this tile (idle columns of a tile in use get zeros)
@@ -1298,7 +1300,8 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
 // Combine: grid (head, sequence, 8 columns), one warp per column for the weights; then thread = channel quad x
 // column for the weighted sums of the parts, and warp = every eighth channel, lane = four dimensions for the
 // back-projection, whose sums meet in shared memory.  A chain of memory round trips (layout, parts), so each
-// step's loads go out together; the basis is in registers and the mean asked for ahead of the wait for the scan.
+// step's loads go out together; the basis is in registers and the mean asked for ahead of the wait for the scan (its
+// CTAs, past their own wait when they let this kernel start, came behind whatever wrote the parameters).
 // ---------------------------------------------------------------------------------------
 constexpr int kTreeCombine = 8;      // columns of a CTA
 constexpr int kTreeParts = 192;      // parts of a unit at most: the scan's CTAs

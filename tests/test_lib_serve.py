@@ -106,3 +106,21 @@ def test_rope_table64():
     assert status(cobra.cobra_rope_table64, 1e4, 16, A + 8, 1 << 20) == EALIGN
     assert status(cobra.cobra_rope_table64, 1e4, 16, A, 1000) == ESPACE
     assert status(cobra.cobra_rope_table64, 1e4, 16, None, 1 << 20) == EINVAL
+
+
+def test_header_names_the_calls_that_read_parameters_early():
+    """Kernels that read the block ahead of their wait for the kernel in front are calls behind which a block must not be
+    written: their names are in the header's paragraph on it."""
+    import os
+    import re
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = lambda *p: open(os.path.join(root, *p)).read()
+    text = re.search(r"must not be written by the kernel directly ahead(.*?)plain stream order", src("include", "cobra.h"), re.S).group(1)
+    early, ordered = text.split("finishes.")
+    for file, kernel, call in (("append_run.cuh", " append_run_kernel(RunArgs", "cobra_append_tokens"),
+                               ("tree.cuh", " tree_project(const TreeArgs", "cobra_tree_attn")):
+        body = src("paper_2609_24298_gb300", "csrc", file)
+        body = body[body.index(kernel):]
+        first = min(body.index(x) for x in ("param_pool(", "head_table(", "tree_head(") if x in body)
+        assert call in (early if first < body.index("grid_dep_wait();") else ordered)
