@@ -45,6 +45,28 @@ __device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8]) {
   }
 }
 
+// Vectors whose squares leave fp32's range (`far`): scaled by the power of two that takes the larger of the largest element
+// and sqrt(eps) to [1, 2), which leaves x / sqrt(mean(x^2) + eps) as it is.  The reciprocal roots, of the others too.
+__device__ __forceinline__ float norm_scaled(float (&lo)[8], float (&hi)[8], float eps, bool far) {
+  float m = sqrtf(eps);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fmaxf(fabsf(lo[i]), fabsf(hi[i])));
+#pragma unroll
+  for (int x = 4; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+  // 2^-k in two factors (k may be -126); an infinite element is left as it is
+  const int k = far && m < INFINITY ? max((int)(__float_as_uint(m) >> 23), 1) - 127 : 0, k1 = k / 2;
+  const float f = __uint_as_float((uint32_t)(127 - k1) << 23), g = __uint_as_float((uint32_t)(127 - (k - k1)) << 23);
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lo[i] = lo[i] * f * g, hi[i] = hi[i] * f * g;
+    ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
+  }
+#pragma unroll
+  for (int x = 4; x; x >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, x);
+  return rsqrtf(fmaf(ss, 1.f / kD, eps * f * f * g * g));
+}
+
 __global__ void __launch_bounds__(kNormThreads, 8) norm_rope_kernel(NormArgs a) {
   grid_dep_launch();
   // the vectors may come from the kernel ahead, or still be read by it where the output goes
@@ -102,7 +124,10 @@ __global__ void __launch_bounds__(kNormThreads, 8) norm_rope_kernel(NormArgs a) 
       for (int i = 0; i < 8; ++i) ss = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], ss));
 #pragma unroll
       for (int m = 4; m; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-      const float inv = rsqrtf(fmaf(ss, 1.f / kD, a.eps));  // (2 units in the last place)
+      const float mean = fmaf(ss, 1.f / kD, a.eps);
+      float inv = rsqrtf(mean);  // (2 units in the last place)
+      const bool far = live && !(mean >= 1e-30f && mean < INFINITY);
+      if (__any_sync(0xffffffffu, far)) inv = norm_scaled(lo, hi, a.eps, far);
       if (sd.w) {
         const float4* w4 = reinterpret_cast<const float4*>(sd.w);
 #pragma unroll
