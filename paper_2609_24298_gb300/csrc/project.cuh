@@ -27,8 +27,6 @@ struct ProjSmem {
   __device__ explicit ProjSmem(float* base)
       : Ws(base), Xs(Ws + kD * kProjLd), Os(Xs + kProjVecs * kD), wmu(Os + kProjVecs * kProjLd),
         pos(reinterpret_cast<int*>(wmu + kD)) {}
-  __device__ ProjSmem(float* ws, float* xs, float* os, float* wmu_, int* pos_)
-      : Ws(ws), Xs(xs), Os(os), wmu(wmu_), pos(pos_) {}
 };
 
 // nv vectors of 128 bf16 into Xs; row(v) is vector v's address.  `wide`: every row is 16-byte

@@ -203,14 +203,9 @@ __device__ __forceinline__ void tc_unpack_v(const uint8_t* src, uint32_t a_tmem,
 // strips j and j + 4 of a tile of 8 strips, one or two words each, so that a word gives four registers (a
 // token per thread would use one code pair of each word).  The registers are stored by 16x256b: lanes g, g + 8
 // of each half of the warp's lanes, columns 2 j and 2 j + 1: column 2 s holds strip s < 4 of a tile, column
-// 2 s + 1 strip s + 4 (tc_k_place).
+// 2 s + 1 strip s + 4 (tc_k_channel).
 // ---------------------------------------------------------------------------------------
-// place of channel ch among the 16 elements of its tile
-__host__ __device__ constexpr int tc_k_place(int ch) {
-  const int s = (ch & 15) >> 1;
-  return (ch & ~15) | (4 * (s & 3) + 2 * (s >> 2) + (ch & 1));
-}
-// and the channel at a place
+// channel at place p of the 16 elements of a tile
 __host__ __device__ constexpr int tc_k_channel(int p) {
   const int c = (p & 15) >> 1;
   return (p & ~15) | (2 * ((c >> 1) + 4 * (c & 1)) + (p & 1));
