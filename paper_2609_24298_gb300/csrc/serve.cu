@@ -213,14 +213,18 @@ size_t tree_layout_host(const cobra_tree_desc* d, unsigned char* base, TreeArgs&
   return off;
 }
 
-template <int NC, int NCW>
-cobra_status launch_tree_scan(const TreeArgs& a, cudaStream_t s) {
+template <int NC, int NCW, bool LARGE>
+cobra_status launch_tree_scan_kind(const TreeArgs& a, cudaStream_t s) {
   using Smem = TreeScanSmem<NC, NCW>;
   static Granted granted;
-  if (ensure_smem(tree_scan_kernel<NC, NCW>, sizeof(Smem) + 1024, granted) != COBRA_OK) return COBRA_ECUDA;
-  return launch_pdl(tree_scan_kernel<NC, NCW>, (unsigned)a.ctas, Smem::kThreads, sizeof(Smem) + 1024, s, a) == cudaSuccess
+  if (ensure_smem(tree_scan_kernel<NC, NCW, LARGE>, sizeof(Smem) + 1024, granted) != COBRA_OK) return COBRA_ECUDA;
+  return launch_pdl(tree_scan_kernel<NC, NCW, LARGE>, (unsigned)a.ctas, Smem::kThreads, sizeof(Smem) + 1024, s, a) == cudaSuccess
              ? COBRA_OK
              : COBRA_ECUDA;
+}
+template <int NC, int NCW>
+cobra_status launch_tree_scan(const TreeArgs& a, cudaStream_t s) {
+  return a.cap2 > kTreeCapPlain ? launch_tree_scan_kind<NC, NCW, true>(a, s) : launch_tree_scan_kind<NC, NCW, false>(a, s);
 }
 
 }  // namespace

@@ -36,6 +36,7 @@ constexpr int kTreeMaxDraft = 64;
 constexpr uint64_t kTreeWaitNs = 2000000000ull;  // 2 s
 constexpr int kTreeChunk = 32;    // columns of a prepare unit
 constexpr int kTreePart = kD + 4;  // floats of a column's partial: m, l, -, -, O[128]
+constexpr float kTreeCapPlain = 512.f;  // caps up to here (log2 units, 355 of a score) take the formula alone: see tree_cap
 constexpr float kTreeLargest = 1e38f;   // magnitude of a score that fp32 holds with its parts
 constexpr float kTreeLowest = -3e38f;   // stands for a drafted score of -inf: below every other, but seen
 constexpr float kTreeBound = 80.f;  // scores this near their reference need no running maximum: 2^80 times codes of 2^7, summed over 2^31 tokens, is finite
@@ -155,16 +156,16 @@ __device__ __forceinline__ int tree_img_at(int nc, int col, int p) {
   return (p >> 6) * nc * 128 + col * 128 + ((((p & 63) >> 3) ^ (col & 7)) << 4) + (p & 7) * 2;
 }
 // z with the cap: cap2 tanh(z / cap2) = cap2 (1 - 2 / (1 + e^{2 z / cap2})).  The difference loses relative, not
-// absolute accuracy near 0: the score is within 2^-20 cap2, for caps up to kTreeBound 2^-13 of a log2 unit.
-__device__ __forceinline__ float tree_cap(float z, float cap2, float k) {  // cap2 <= kTreeBound, k = tree_cap_k
+// absolute accuracy near 0: the score is within 2^-20 cap2, for caps up to kTreeCapPlain 2^-11 of a log2 unit.
+__device__ __forceinline__ float tree_cap(float z, float cap2, float k) {  // cap2 <= kTreeCapPlain, k = tree_cap_k
   return cap2 - __fdividef(2.f * cap2, 1.f + ex2_approx(z * k));
 }
 __device__ __forceinline__ float tree_cap_k(float cap2) {  // 2 log2e / cap2, finite (0 times it has to be 0)
   return cap2 > 0.f ? fminf(__fdiv_rn(2.f * kLog2e, cap2), 3e38f) : 0.f;
 }
-// The same for any cap (with one of 1e5 the above would be off by 0.1): below 0.3 cap2 the series of tanh to x^9, whose
+// The same for larger caps (with one of 1e5 the above would be off by 0.1): below 0.3 cap2 the series of tanh to x^9, whose
 // rest is below 2^-24 of it, so that the result is within 2^-19 of itself.
-__device__ __forceinline__ float tree_cap_any(float z, float cap2, float k) {
+__device__ __forceinline__ float tree_cap_large(float z, float cap2, float k) {
   const float x = z * k * (0.5f / kLog2e), x2 = x * x;
   const float series = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
   return fabsf(x) < 0.3f ? z * series : tree_cap(z, cap2, k);
@@ -506,7 +507,7 @@ __device__ __forceinline__ void tree_draft_part(const TreeArgs& a, TreeDraftSmem
       const long long dist = (long long)sm.pos[j] - sm.pos[i];
       const bool seen = (sm.mask[i] >> j & 1ull) != 0ull && (a.window <= 0 || dist > -(long long)a.window);
       float y = z[u >> 1][u & 1];
-      if (a.cap2 > 0.f) y = tree_cap_any(y, a.cap2, k2);
+      if (a.cap2 > 0.f) y = a.cap2 <= kTreeCapPlain ? tree_cap(y, a.cap2, k2) : tree_cap_large(y, a.cap2, k2);
       if (a.slopes) y = fmaf(a.slopes[kv * G + g] * kLog2e, (float)dist, y);
       sm.z[c][j] = !seen ? -INFINITY : y < kTreeLowest ? kTreeLowest : y;
     }
@@ -762,9 +763,9 @@ __device__ __forceinline__ float tree_reduce(float (&v)[N], Op op) {
   }
   return v[0];
 }
-// Scores of the thread's token against the columns: absolute (log2 units) or less the reference.  A column
-// without a reference has sub = +3e38 (plain) or -3e38 (ref), so that any score it sees asks for one.
-template <int NCW, bool ABS, bool BOUNDED>
+// Scores of the thread's token against the columns: absolute (log2 units) or less the reference.  A column without a
+// reference has sub = +3e38 (plain) or -3e38 (ref), so that any score it sees asks for one.
+template <int NCW, bool ABS, bool LARGE>
 __device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>& w, const uint32_t (&x)[NCW], float k2,
                                             bool plain, bool masked, int tok, float (&z)[NCW]) {
   if (plain) {
@@ -781,7 +782,7 @@ __device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>
 #pragma unroll
     for (int j = 0; j < NCW; ++j) {
       float y = __uint_as_float(x[j]) + w.c0[j];
-      if (a.cap2 > 0.f) y = BOUNDED ? tree_cap(y, a.cap2, k2) : tree_cap_any(y, a.cap2, k2);
+      if (a.cap2 > 0.f) y = LARGE ? tree_cap_large(y, a.cap2, k2) : tree_cap(y, a.cap2, k2);
       if (a.slopes) y = fmaf(w.slope[j], (float)(tok - w.pos[j]), y);
       z[j] = ABS ? y : y - w.sub[j];
     }
@@ -793,7 +794,9 @@ __device__ __forceinline__ void tree_scores(const TreeArgs& a, const TreeWg<NCW>
   }
 }
 
-template <int NC, int NCW>
+// LARGE: caps above kTreeCapPlain (a kernel of their own: with both formulas in one, calls with biases and loud queries
+// took 142 us for 111, 32 ragged sequences of up to 16384 tokens)
+template <int NC, int NCW, bool LARGE>
 __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_kernel(TreeArgs a) {
   using Smem = TreeScanSmem<NC, NCW>;
   constexpr int kWg = Smem::kWg, kMmaWarp = 8 + 4 * kWg;
@@ -1058,7 +1061,8 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
       if (!ok || !more) break;
       const TreeCol* col = sm.col[seg & 1] + wg * NCW;
       const int live = min(NCW, d.n_col - wg * NCW);  // may be <= 0
-      const bool bounded = col[0].bounded > 0;
+      const int kind = col[0].bounded;
+      const bool bounded = kind > 0;
       if (t < NCW) {
         const TreeCol c = col[t];
         w.c0[t] = c.c0;
@@ -1150,26 +1154,35 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
           arrive(p_ready);
           continue;
         }
+        // a chunk with scaled columns: the scales taken off S in place, in little code (as part of tree_scores, loud queries
+        // on 64 columns take 149 us for 136, 8 x 32768 tokens, where no column is scaled either)
+        if (kind < 0 && d.rk > 0) {
+          const uint32_t at = tmem + lanes + kS + 64 * u + wg * NCW;
+#pragma unroll 1
+          for (int c = 0; c < NCW; c += 8) {
+            uint32_t x[8];
+            tree_ld<8>(at + c, x);
+            tree_wait_ld<8>(x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * w.sc[c + i]);
+            tree_st<8>(at + c, x);
+          }
+          tc_wait_st();
+        }
         float z[NCW];
         auto load = [&](auto use) {
           uint32_t x[NCW];
           if (d.rk > 0) {
             tree_ld<NCW>(tmem + lanes + kS + 64 * u + wg * NCW, x);
             tree_wait_ld<NCW>(x);
-            if (col[0].bounded < 0) {
-#pragma unroll
-              for (int j = 0; j < NCW; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * w.sc[j]);
-            }
           } else {
 #pragma unroll
             for (int j = 0; j < NCW; ++j) x[j] = 0u;
           }
           use(x);
         };
-        auto scores = [&](auto abs, auto bnd) {
-          load([&](const uint32_t(&x)[NCW]) {
-            tree_scores<NCW, decltype(abs)::value, decltype(bnd)::value>(a, w, x, k2, plain, masked, tok, z);
-          });
+        auto scores = [&](auto abs) {
+          load([&](const uint32_t(&x)[NCW]) { tree_scores<NCW, decltype(abs)::value, LARGE>(a, w, x, k2, plain, masked, tok, z); });
         };
         float top = -INFINITY;
         if (bounded && plain) {
@@ -1182,16 +1195,16 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
             for (int j = 0; j < NCW; ++j)
               if (tok < w.lo[j] || tok >= w.hi[j]) z[j] = -INFINITY;
           }
-        } else if (bounded) {
-          scores(std::false_type{}, std::true_type{});
         } else {
-          scores(std::false_type{}, std::false_type{});
+          scores(std::false_type{});
+          if (!bounded) {
 #pragma unroll
-          for (int j = 0; j < NCW; ++j) top = fmaxf(top, z[j]);
+            for (int j = 0; j < NCW; ++j) top = fmaxf(top, z[j]);
+          }
         }
         if (!bounded && wg_any(wg, top > kTreeTau)) {
           // the columns' maxima over the row, new references where they are exceeded
-          scores(std::true_type{}, std::false_type{});
+          scores(std::true_type{});
           const float mine = tree_reduce<NCW>(z, [](float p, float q) { return fmaxf(p, q); });
           w.red[wq][tree_owned<NCW>(lane)] = mine;
           wg_sync(wg);
@@ -1222,7 +1235,7 @@ __global__ void __launch_bounds__(TreeScanSmem<NC, NCW>::kThreads, 1) tree_scan_
             }
             tc_wait_st();
           }
-          scores(std::false_type{}, std::false_type{});
+          scores(std::false_type{});
         }
         tc_fence_before();
         arrive(sm.s_ready[u]);  // for the row after the next
