@@ -447,8 +447,8 @@ typedef struct {
  * fp32 with one rounding to bf16.  q_weight / k_weight: device fp32 [128] shared by the side's heads, or
  * NULL for ones.  pos: device int32 [n_tok]; rope_table / max_pos: a table from cobra_rope_table, R as for
  * cobra_decode_rope_attn, or NULL for no rotation (a position outside the table is reported through the
- * device status word and uses the nearest angles).  An output may be its input, with the same strides;
- * otherwise they must not overlap.  One launch.  Errors: EINVAL, EALIGN (vectors and outputs 16-byte
+ * device status word and uses the nearest angles).  Vectors may be of any size that bf16 holds, with eps = 0
+ * too.  An output may be its input, with the same strides; otherwise they must not overlap.  One launch.  Errors: EINVAL, EALIGN (vectors and outputs 16-byte
  * aligned, strides multiples of 8, weights and table 16-byte aligned), ECUDA. */
 cobra_status cobra_norm_rope(const cobra_norm_rope_desc* desc, const void* q, const void* k, const float* q_weight,
                              const float* k_weight, const int* pos, const float* rope_table, int max_pos, void* q_out,
@@ -507,7 +507,9 @@ typedef struct {
 } cobra_tree_desc;
 
 /* Workspace bytes of cobra_tree_attn on the current device (they depend on the descriptor's counts alone,
- * not on lengths). */
+ * not on lengths).  They grow with n_layers * n_kv_heads * n_seqs * max_draft * group, about 1.3 KB for each: 11 MB
+ * for a layer of 8 kv heads x 4 query heads, 16 sequences and 16 drafted tokens, gigabytes for all layers of a
+ * model in one call; calls per layer, one after another, can share one. */
 cobra_status cobra_tree_workspace_size(const cobra_tree_desc* desc, size_t* bytes);
 
 /* Attention of up to max_draft query tokens per sequence over the packed cache, and over one another's
@@ -516,7 +518,7 @@ cobra_status cobra_tree_workspace_size(const cobra_tree_desc* desc, size_t* byte
  * over the cached tokens t < seq_lens[s] (keys and values as in cobra_decode_attn, means included; key t at
  * position t) with p_i - window < t <= p_i, and the drafted tokens j < n_draft[s] whose bit (i, j) of
  * tree_mask is set (within the window too).  A token that sees nothing gets zeros; NaN and infinities of
- * queries, drafted keys and values or slopes reach what sees them as they do in the formula (scores that are not
+ * queries, drafted keys and values or slopes reach what sees them as they do in the formula (queries and scores that are not
  * finite give NaN), and nothing else.
  *   q          device bf16, token i, query head j at q[l*sl + s*ss + i*st + j*128]
  *   k_draft, v_draft  device bf16 (rotated like the cache's keys), or both NULL: queries see the cache
@@ -527,9 +529,11 @@ cobra_status cobra_tree_workspace_size(const cobra_tree_desc* desc, size_t* byte
  *   q_pos      device int32 [n_seqs][max_draft] positions p_i, or NULL: seq_lens[s] + i
  *   slopes     device fp32 [n_kv_heads * group] distance biases per query head, or NULL
  *   out        device bf16; the softmax and all sums are in fp32 or wider
- * Queries enter the matrix products as f16 (a rounding of 2^-12 per element, below that of the bf16 query
- * itself; vectors that would overflow are scaled by a power of two first), probabilities as bf16 (2^-9), whose
- * sum is that of the rounded ones.
+ * Projected queries enter the matrix products as f16 (each element rounded by 2^-11 of it at most; a query whose
+ * elements would overflow is scaled by a power of two of its own), probabilities of cached tokens as bf16 (2^-8),
+ * whose sum is that of the rounded ones: about 1.1e-3 of a result, next to the 1.7e-3 of its own rounding to bf16.
+ * Any cap may be given; calls take longer where neither a cap up to 55 nor the queries bound the scores to 2^80
+ * of one another (queries several times as long as their keys' usual ones).
  * Three launches; nothing is synchronised, and the workspace (256-byte aligned) carries nothing from call to
  * call: calls that overlap need one each.  Lengths outside the cache, counts outside 0 .. max_draft and heads
  * the block does not hold are clamped and reported (cobra_check returns COBRA_EINVAL).  Errors: EINVAL,

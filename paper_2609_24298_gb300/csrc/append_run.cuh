@@ -22,7 +22,7 @@
 // read and write, because nobody else has the row.
 //
 // What bounds it: chains of memory round trips per batch (positions, vectors and angles, products, codes, words),
-// and the instructions that turn and split keys.  32 layers x 8 kv heads x 64 sequences x 4 tokens, K turned: 127 us,
+// and the instructions that turn and split keys.  32 layers x 8 kv heads x 64 sequences x 4 tokens, K turned: 128 us,
 // of whose touched sectors 200 MB have to move (30 us); 2001 tokens of a layer 29 us; 304 and 61 with the projection
 // in fp32 on the CUDA cores.
 #pragma once

@@ -294,7 +294,7 @@ struct TreeProjSmem {
 };
 
 // q~ and c0 of 32 columns.  The projection is a product of bf16 queries with the basis in two bf16 pieces, summed
-// in fp32: 2^-18 |w| |q| off by the pieces and as much by the sums (append_run.cuh), below the 2^-12 of an element
+// in fp32: 2^-17 |w| |q| off by the pieces and half as much by the sums (append_run.cuh), below the 2^-11 of an element
 // that f16 takes.  (In fp32 on the CUDA cores, bound by shared-memory reads, the product alone took 4.3 us.)
 __device__ __forceinline__ void tree_project(const TreeArgs& a, TreeProjSmem& sm, int head, int s, int chunk) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -632,20 +632,21 @@ struct TreeWalk {
 //                memory: rows of 64 columns per token, the MN-major operand of the second product
 // KA, VA and S have two buffers and P three, so that a row's five steps run beside those of its neighbours.
 //
-// The fed probabilities 2^(z - reference) are bf16 (a rounding of 2^-9, as the result's own; the sums l are of
-// the fed values, so the weights are normalised exactly): its exponents hold all that fp32 does, so the
+// The fed probabilities 2^(z - reference) are bf16 (a rounding of 2^-8, as the result's own; the sums l are of
+// the fed values, so the weights are normalised exactly; it makes the result 1.1e-3 less exact than f16 would): its exponents hold all that fp32 does, so the
 // reference need not follow the maximum.  Where the codes bound the scores to within kTreeBound of c0 (or a cap
 // bounds them), c0 (0) and the largest bias are the reference, a score goes from TMEM into the exponential as it is
 // (or capped and with its bias), and the warps of a row need not agree on anything.  Else (large queries) a
 // reference is raised when a score
-// exceeds it by kTreeTau (one vote per row and 32 columns), and the columns' sums and O are rescaled.  64 columns,
-// 131072 tokens at 0.5 bpd: 306 us a call with this, 359 with f16 probabilities and votes (295 with the later steps).
+// exceeds it by kTreeTau (one vote per row and 32 columns), and the columns' sums and O are rescaled.  Queries of standard
+// deviation 1.5, bounded, and 4, with votes: 64 columns, 131072 tokens at 0.5 bpd 284 and 397 us a call; 8 x 32768 at
+// 1 bpd 107 and 136; single tokens with biases over 32 ragged sequences of up to 16384 at 4 bpd 74 and 111.
 //
 // What bounds it: a row takes 1300 to 1600 cycles, of which the products' own are 80 (16 columns) to 512.  The issue
 // slots of an SM's four quarters are used to 0.61 on average and to 0.74 in the fullest: the K, V and softmax warps of
 // the same 32 TMEM lanes share one, and ranks up to 64 leave two quarters without V codes.  The rest are the two
-// chains of hand-overs (product, softmax, next product into the same buffer; codes, product, next codes): with the
-// unpacking left out the case above takes 260 us, with the exponentials left out too 244.
+// chains of hand-overs (product, softmax, next product into the same buffer; codes, product, next codes): when the first
+// case above took 306 us, it took 260 with the unpacking left out and 244 with the exponentials left out too.
 // ---------------------------------------------------------------------------------------
 constexpr float kTreeTau = 60.f;
 constexpr int kTreeRingBytes = 57344;    // K rows in flight, and V rows: as many as fit, 3 of the largest at least
