@@ -10,10 +10,11 @@ from .serve_util import D
 
 
 def close_check(call, pos, pairs=None, may_be_wrong=()):
-    """Within the close bound at the (kv head, sequence) pairs (None: all); and each of `may_be_wrong`, a change
+    """Within the close bound at the (kv head, sequence) pairs of the first layer (None: all); and each of `may_be_wrong`, a change
     of (length, positions, window), breaks it somewhere."""
     assert cobra.cobra_check() == cobra.COBRA_OK
     c, G = call.c, call.G
+    v0 = c.layers * c.kv
     o = call.o_v.double().cpu().numpy()
     broken = [False] * len(may_be_wrong)
     for h, s in pairs or [(h, s) for h in range(c.kv) for s in range(call.S)]:
@@ -21,8 +22,8 @@ def close_check(call, pos, pairs=None, may_be_wrong=()):
 
         def want(n, T, p, window):
             kd, vd = (x[0, s, :n, h] if call.drafts else None for x in (call.kd, call.vd))
-            return serve.tree_attend_close(call.q[0, s, :n, h * G:(h + 1) * G], c.codes[h, s][:T], c.codes[c.kv + h, s][:T],
-                                           c.params[h], c.params[c.kv + h], kd, vd,
+            return serve.tree_attend_close(call.q[0, s, :n, h * G:(h + 1) * G], c.codes[h, s][:T], c.codes[v0 + h, s][:T],
+                                           c.params[h], c.params[v0 + h], kd, vd,
                                            None if call.mask is None else call.mask[s][:n, :n], p, window, call.cap,
                                            None if call.slopes is None else call.slopes[h * G:(h + 1) * G])
 
